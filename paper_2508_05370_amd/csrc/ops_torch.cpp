@@ -277,7 +277,7 @@ py::tuple norm(const Tensor& h, const Maybe& y, const Maybe& gate, const Maybe& 
 
 py::tuple norm_backward(const Maybe& dh, const Maybe& dx, const Tensor& h, const Maybe& y, const Maybe& gate, const Maybe& post_weight,
                         const Maybe& post_bias, const Maybe& pre_weight, const Maybe& post_stats, const Maybe& pre_stats, int post,
-                        int pre, double alpha, double beta, const std::optional<int64_t>& rows_per_gate) {
+                        int pre, double alpha, double beta, const std::optional<int64_t>& rows_per_gate, const Maybe& pre_bias) {
   require(y || dx, "y or dx is there");
   const at::ScalarType act_type = y ? y->scalar_type() : dx->scalar_type();
   const int act = type_of(act_type);
@@ -324,7 +324,10 @@ py::tuple norm_backward(const Maybe& dh, const Maybe& dx, const Tensor& h, const
   a.post_bias = vector_of(at, post_bias, m.cols, "post_bias");
   a.pre_weight = vector_of(at, pre_weight, m.cols, "pre_weight");
   a.dh = out.data_ptr(); a.ld_dh = m.cols;
-  const bool wanted[4] = {post != SIM_NORM_NONE, post == SIM_NORM_LAYER, pre != SIM_NORM_NONE, pre == SIM_NORM_LAYER};
+  // a bias has a gradient after a layer norm, and wherever the forward pass took one (its values count in dgate alone)
+  const bool post_sum = post == SIM_NORM_LAYER || (post != SIM_NORM_NONE && a.post_bias);
+  const bool pre_sum = pre == SIM_NORM_LAYER || (pre != SIM_NORM_NONE && vector_of(at, pre_bias, m.cols, "pre_bias"));
+  const bool wanted[4] = {post != SIM_NORM_NONE, post_sum, pre != SIM_NORM_NONE, pre_sum};
   float** places[4] = {&a.dpost_weight, &a.dpost_bias, &a.dpre_weight, &a.dpre_bias};
   for (int i = 0; i < 4; ++i)
     if (wanted[i]) {

@@ -114,12 +114,13 @@ def norm_block(h, y=None, gate=None, post_weight=None, post_bias=None, pre_weigh
 
 
 def norm_block_backward(dh, dx, h, y=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, post_stats=None,
-                        pre_stats=None, post="none", pre="rms", alpha=1.0, beta=1.0, rows_per_gate=None):
+                        pre_stats=None, post="none", pre="rms", alpha=1.0, beta=1.0, rows_per_gate=None, pre_bias=None):
     """Gradients of norm_block from those of its h (dh, None: zero) and its x (dx; None with pre="none"): h is its output h, the
-    other arguments are its own and its statistics.  Returns NormGrad; what the forward pass had no input for is None (the
-    weights' and biases' gradients are there for every norm, in 32 bits like dgate)."""
+    other arguments are its own and its statistics.  Returns NormGrad; what the forward pass had no input for is None.  The
+    weights' gradients are there for every norm, the biases' for every layer norm and for an rms norm whose bias is given here
+    as it was to norm_block; all of them in 32 bits, like dgate."""
     return NormGrad._make(_ops.norm_backward(dh, dx, h, y, gate, post_weight, post_bias, pre_weight, post_stats, pre_stats,
-                                             _kind(post), _kind(pre), alpha, beta, rows_per_gate))
+                                             _kind(post), _kind(pre), alpha, beta, rows_per_gate, pre_bias))
 
 
 # ---------------------------------------------------------------- AdamW

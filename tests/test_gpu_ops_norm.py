@@ -288,3 +288,36 @@ def test_places_past_32_bits():
     # the other rows have no gradient of their own: the sums are the last rows', in another order
     assert torch.allclose(ga.dpre_weight, gb.dpre_weight, rtol=1e-5, atol=1e-4)
     assert torch.allclose(ga.dpost_weight, gb.dpost_weight, rtol=1e-5, atol=1e-4)
+
+
+@pytest.mark.parametrize("post,pre", [("rms", "rms"), ("rms", "layer"), ("layer", "rms"), ("none", "rms"), ("rms", "none")])
+@pytest.mark.parametrize("rows,hidden,gate", [(1, 8, "none"), (3, 100, "channel"), (70, 129, "sequence"), (600, 64, "token"),
+                                              (33, 768, "sequence"), (5, 4096, "channel"), (3, 12288, "sequence")])
+def test_bias_gradients(rows, hidden, gate, post, pre):
+    """A bias that the forward pass took has a gradient, after whatever kind of norm it came."""
+    act, res = torch.bfloat16, torch.float32
+    c = _case(rows, hidden, post, pre, gate, act, res, seed=21)
+    dh, dx = _normal(5, rows, hidden, dtype=res), _normal(6, rows, hidden, dtype=act) if pre != "none" else None
+    c["h"] = h_out = _grad64(c, post, "none", 0.9, 0.7, dh, None)[0].to(res)
+    d = dh.double()
+    if pre != "none":
+        leaf, qw, qb = (v.double().requires_grad_() for v in (h_out, c["qw"], c["qb"]))
+        ((_norm64(leaf, pre) * qw + qb) * dx.double()).sum().backward()
+        d = d + leaf.grad
+    want = _grad64(c, post, "none", 0.9, 0.7, d, None)[1]
+    r = ops.norm_block_backward(dh, dx, h_out, c["y"], gate=c["gate"], post_weight=c["pw"], post_bias=c["pb"], pre_weight=c["qw"],
+                                pre_bias=c["qb"], post_stats=_stats(c["y"].double(), post), pre_stats=_stats(h_out.double(), pre),
+                                post=post, pre=pre, alpha=0.9, beta=0.7, rows_per_gate=c["per"])
+    scale = 8.0 + sum(float(want[k].abs().amax()) for k in ("h", "y"))
+    # sums over the rows, as in test_backward
+    terms = 4.0 * scale * scale * (rows ** 0.5 + 4.0)
+    for got, true in ((r.dpost_bias, want.get("pb")), (r.dpost_weight, want.get("pw")), (r.dgate, want.get("gate"))):
+        assert (got is None) == (true is None)
+        if true is not None:
+            _close(got, true, ULP[torch.float32], terms)
+    assert (r.dpre_bias is None) == (pre == "none")
+    if pre != "none":
+        _close(r.dpre_bias, qb.grad, ULP[torch.float32], terms)
+        _close(r.dpre_weight, qw.grad, ULP[torch.float32], terms)
+    _close(r.dh, want["h"], ULP[res], scale)
+    _close(r.dy, want["y"], ULP[act], scale)
