@@ -235,3 +235,31 @@ def test_places_past_32_bits():
     want = _step64(before, g[first:].double(), 0.0, 0.0, 1, 0.0)[0]
     assert ((p[first:].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20 * 0.1).all()
     assert float(p[:first].abs().amax()) == 0.0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -130, 1e-30, 1e-20])
+def test_small_gradients_and_small_eps(bits, eps):
+    """Second moments below the smallest normal number, and denominators near it: the first step moves a parameter by
+    lr g / (|g| + eps), and by nothing where g is zero (unless that is 0 / 0)."""
+    n = 128
+    g = torch.cat([torch.logspace(-23, -12, n - 1), torch.zeros(1)]).cuda()
+    p, moments = [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda") for _ in range(2)]
+    scales = None
+    if bits == 8:
+        (moments[0], ms), (moments[1], vs) = _eight(moments[0]), _eight(moments[1])
+        scales = dict(exp_avg_scales=[ms], exp_avg_sq_scales=[vs])
+    ops.adamw(p, [g], moments[:1], moments[1:], step=1, weight_decay=0.0, lr=1e-2, beta1=0.5, beta2=0.75, eps=eps, **(scales or {}))
+    d, v = g.double(), 0.25 * g.double().square()
+    want = -1e-2 * d / (d + eps)
+    if eps == 0.0:
+        assert torch.isnan(p[0][-1])
+        want[-1] = p[0][-1] = 0.0
+    # v is a whole number of 2^-149 here: the root's error is that of v, half a spacing of 0.25 g^2 (after g * 0.25's own rounding)
+    loss = (2.0 ** -149 / v.clamp_min(2.0 ** -300)).clamp_max(1e30) + 2.0 ** -20
+    sure = v > 2.0 ** -146
+    assert ((p[0].double() - want).abs() <= 1e-2 * loss)[sure].all()
+    assert (p[0][:-1] <= 0).all() and p[0][-1] == 0.0
+    if eps:
+        # where v is zero the quotient is m / eps, however v is rounded an update of at most lr g / eps
+        assert (p[0].double().abs() <= 1e-2 * d / eps * 1.001 + 1e-30).all()
