@@ -227,11 +227,17 @@ __global__ __launch_bounds__(kThreads) void k_norm(Fwd p, int per_row, int rows_
       if (p.q) {
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(w[i]));
+        for (int i = 0; i < 8; ++i) {
+          if (!kVec && i >= have[j]) w[i] = 0.0f;
+          m = fmaxf(m, fabsf(w[i]));
+        }
         m = fmaxf(max16(m), kAmaxFloor);
         const float f = kE4m3Max / m;
         if (c[j] < ((int)p.hidden + kBlock - 1) / kBlock * kBlock) {
-          *(u32x2*)(p.q + row * p.ld_q + c[j]) = u32x2{codes4(w[0], w[1], w[2], w[3], f), codes4(w[4], w[5], w[6], w[7], f)};
+          // (zero past the row also where an infinite or NaN rstd has made NaN of its zeros)
+          const uint32_t in = !kVec || have[j] > 0 ? ~0u : 0u;
+          *(u32x2*)(p.q + row * p.ld_q + c[j]) =
+              u32x2{codes4(w[0], w[1], w[2], w[3], f) & in, codes4(w[4], w[5], w[6], w[7], f) & in};
           if ((tr & 15) == 0) p.s[c[j] / kBlock * p.ld_s + row] = m / kE4m3Max;
         }
       } else {

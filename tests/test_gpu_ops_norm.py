@@ -321,3 +321,22 @@ def test_bias_gradients(rows, hidden, gate, post, pre):
         _close(r.dpre_weight, qw.grad, ULP[torch.float32], terms)
     _close(r.dh, want["h"], ULP[res], scale)
     _close(r.dy, want["y"], ULP[act], scale)
+
+
+@pytest.mark.parametrize("hidden", [8, 200, 131, 1000, 4100, 12290])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_padding_of_not_finite_rows(hidden, kind):
+    """The codes past a row's end are zero, whatever the row holds."""
+    h = _normal(1, 9, hidden)
+    h[1, 3] = float("nan")
+    h[2, 5] = float("inf")
+    h[4] = float("nan")
+    h[6, hidden - 1] = float("-inf")
+    q = ops.norm_block(h, pre=kind, eps=EPS, quantized=True)
+    assert q.x.shape[1] > hidden and int(q.x[:, hidden:].view(torch.uint8).amax()) == 0
+    y = torch.zeros_like(h)
+    q = ops.norm_block(y, h, post=kind, pre=kind, eps=EPS, quantized=True)
+    assert int(q.x[:, hidden:].view(torch.uint8).amax()) == 0
+    # zero rows with eps = 0 are 0 / 0
+    q = ops.norm_block(y, pre=kind, eps=0.0, quantized=True, pre_bias=_normal(2, hidden))
+    assert torch.isnan(q.x[:, :hidden].float()).all() and int(q.x[:, hidden:].view(torch.uint8).amax()) == 0
