@@ -281,7 +281,7 @@ extern "C" int sim_op_adamw(const sim_adamw_tensor* tensors, int64_t n, const si
   int64_t chunks = 0;
   // as many tensors to a launch as its table and its grid hold; a tensor of
   // more chunks than a grid has goes in several pieces
-  constexpr int64_t kGrid = (int64_t)1 << 30;
+  constexpr int64_t kGrid = most_groups(kThreads);
   for (int64_t i = 0; i < n; ++i) {
     int64_t done = 0;
     while (done < tensors[i].n) {

@@ -117,6 +117,9 @@ __device__ inline float sum64(float v) {
   return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
 
+// Workgroups that one launch may have: it counts its threads in 32 bits.
+constexpr int64_t most_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+
 inline hipError_t launched() { return hipGetLastError(); }
 
 // A block form that a call reads or writes: rows x cols elements.

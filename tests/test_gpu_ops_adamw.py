@@ -263,3 +263,23 @@ def test_small_gradients_and_small_eps(bits, eps):
     if eps:
         # where v is zero the quotient is m / eps, however v is rounded an update of at most lr g / eps
         assert (p[0].double().abs() <= 1e-2 * d / eps * 1.001 + 1e-30).all()
+
+
+def test_more_chunks_than_a_launch_takes():
+    """A launch counts its threads in 32 bits, which is 2^24 - 1 chunks of 2048 elements: the rest goes into another.  The boundary
+    lies inside a tensor of three chunks here; what fills the first launch is one tensor many times over, which a step with both
+    betas and the rate zero leaves as it is after the first time (m = g, v = g^2)."""
+    n, chunk, limit = 1 << 30, 2048, (1 << 24) - 1
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    m, v = (torch.zeros(n, device="cuda") for _ in range(2))
+    g[-1] = 3.0
+    full, rest = limit * chunk // n, limit % (n // chunk) - 1       # the last chunk of the first launch is left for the small tensor
+    sizes = [n] * full + [rest * chunk, 3 * chunk - 5, 700]
+    small = [(_normal(i, k, dtype=torch.bfloat16), _normal(9 + i, k, dtype=torch.bfloat16), _normal(20 + i, k), _normal(30 + i, k).square())
+             for i, k in enumerate(sizes[-2:])]
+    want = [g64[1].double() for g64 in small]
+    lists = [[big] * full + [big[:rest * chunk]] + [s[i] for s in small] for i, big in enumerate((p, g, m, v))]
+    ops.adamw(*lists, step=1, lr=0.0, beta1=0.0, beta2=0.0, eps=1e-8)
+    for (_, gs, ms, vs), w in zip(small, want):
+        assert torch.equal(ms.double(), w) and torch.equal(vs, gs.float().square())
+    assert float(m[-1]) == 3.0 and float(v[-1]) == 9.0 and float(p.abs().amax()) == 0.0 and int(m.count_nonzero()) == 1
