@@ -151,26 +151,41 @@ __global__ __launch_bounds__(256) void k_quant_tile(const T* __restrict__ x, int
   }
 }
 
+// Rows past what one launch takes go into further ones, whole tiles of 128 where
+// it takes tiles.
 template <typename T>
 hipError_t quantize(const T* x, int64_t rows, int64_t cols, int64_t ld, const sim_blocks* q, const sim_blocks* qt,
                     hipStream_t st) {
   const bool vec = aligned(x, 8 * sizeof(T)) && cols % 8 == 0 && ld % 8 == 0;
-  const uint32_t block_rows = q ? q->block_rows : qt->block_rows;
-  if (block_rows == 1 && !qt) {
-    const int64_t grid = cdiv(rows * cdiv(cols, kBlock), 16);
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    auto k = vec ? k_quant_rows<T, true> : k_quant_rows<T, false>;
-    k<<<dim3((uint32_t)grid), 256, 0, st>>>(x, rows, cols, ld, q->codes, q->ld, q->scales, q->ld_s);
-    return launched();
+  const int64_t block_rows = q ? q->block_rows : qt->block_rows, kb = cdiv(cols, kBlock);
+  const bool units = block_rows == 1 && !qt;      // a group of 16 threads to a block of a row, or a workgroup to a tile
+  const int64_t most = units ? most_groups(256) * 16 / kb : most_groups(256) / kb * kBlock;
+  if (most == 0) return hipErrorInvalidValue;
+  sim_blocks a = q ? *q : sim_blocks(), b = qt ? *qt : sim_blocks();
+  for (int64_t r = 0; r < rows; r += most) {
+    const int64_t n = rows - r < most ? rows - r : most;
+    if (units) {
+      auto k = vec ? k_quant_rows<T, true> : k_quant_rows<T, false>;
+      k<<<dim3((uint32_t)cdiv(n * kb, 16)), 256, 0, st>>>(x, n, cols, ld, a.codes, a.ld, a.scales, a.ld_s);
+    } else {
+      auto k = block_rows == 1 ? (vec ? k_quant_tile<T, true, 1> : k_quant_tile<T, false, 1>)
+                               : (vec ? k_quant_tile<T, true, kBlock> : k_quant_tile<T, false, kBlock>);
+      k<<<dim3((uint32_t)(cdiv(n, kBlock) * kb)), 256, 0, st>>>(x, n, cols, ld, a.codes, a.ld, a.scales, a.ld_s, b.codes, b.ld,
+                                                                b.scales, b.ld_s);
+    }
+    const hipError_t e = launched();
+    if (e != hipSuccess) return e;
+    x += n * ld;
+    if (q) {
+      a.codes += n * a.ld;
+      a.scales += n / block_rows;
+    }
+    if (qt) {
+      b.codes += n;
+      b.scales += n / kBlock * b.ld_s;
+    }
   }
-  const int64_t grid = cdiv(rows, kBlock) * cdiv(cols, kBlock);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  auto k = block_rows == 1 ? (vec ? k_quant_tile<T, true, 1> : k_quant_tile<T, false, 1>)
-                           : (vec ? k_quant_tile<T, true, kBlock> : k_quant_tile<T, false, kBlock>);
-  k<<<dim3((uint32_t)grid), 256, 0, st>>>(x, rows, cols, ld, q ? q->codes : nullptr, q ? q->ld : 0,
-                                          q ? q->scales : nullptr, q ? q->ld_s : 0, qt ? qt->codes : nullptr,
-                                          qt ? qt->ld : 0, qt ? qt->scales : nullptr, qt ? qt->ld_s : 0);
-  return launched();
+  return hipSuccess;
 }
 
 hipError_t quantize_any(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, const sim_blocks* q,
@@ -455,8 +470,9 @@ __global__ __launch_bounds__(256) void k_join(Product p, int tiles_m, int tiles_
 }
 
 __global__ __launch_bounds__(256) void k_zero(Product p) {
-  const int64_t per_row = (p.n + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at < p.m * per_row) put4_any(p, at / per_row, at % per_row * 4, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  const int64_t per_row = (p.n + 3) / 4;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < p.m * per_row; at += (int64_t)gridDim.x * 256)
+    put4_any(p, at / per_row, at % per_row * 4, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
 }
 
 // The parts of a split k_few, [splits][m][n in whole fours], in their order.
@@ -682,6 +698,18 @@ bool rounds_itself(int64_t m, int64_t n, int64_t k) {
 }
 
 hipError_t launch_few(Product p, hipStream_t st) {
+  // more rows of B than one launch takes: several (they are not split along k)
+  constexpr int64_t kMost = most_groups(kFewWaves * 64) / 8 * kBlock;
+  while (p.n > kMost) {
+    Product part = p;
+    part.n = kMost;
+    const hipError_t e = launch_few(part, st);
+    if (e != hipSuccess) return e;
+    p.n -= kMost;
+    p.b += kMost * p.ldb;
+    p.bs += kMost >> p.b_shift;
+    p.c = (char*)p.c + kMost * type_bytes(p.c_dtype);
+  }
   split_few(p);
   const Few<uint8_t> few = {p.a, p.lda};
   // 32 rows of B to a wave halve the reads of A; taken where 16 are more than a
@@ -746,7 +774,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k) {
     const int64_t side = tile == 0 ? 256 : 128, slots = tile == 0 ? 256 : 512;
     const double step = tile == 0 ? 1.8 : 1.1;
     const int64_t tiles = cdiv(m, side) * cdiv(n, side), rounds = tiles / slots, left = tiles % slots;
-    if (tiles > INT32_MAX) continue;
+    if (tiles + slots > most_groups(tile == 0 ? 512 : 256)) continue;
     auto consider = [&](int64_t whole, int64_t splits, double us) {
       if (best.us == 0.0 || us < best.us) best = {tile, (int)whole, (int)splits, us};
     };
@@ -768,8 +796,7 @@ hipError_t product(Product p, hipStream_t st) {
   if (p.kb == 0) {
     if (p.accumulate) return hipSuccess;
     const int64_t grid = cdiv(p.m * cdiv(p.n, 4), 256);
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    k_zero<<<dim3((uint32_t)grid), 256, 0, st>>>(p);
+    k_zero<<<dim3((uint32_t)(grid < 65536 ? grid : 65536)), 256, 0, st>>>(p);
     return launched();
   }
   if (p.m <= kFewRows) return launch_few(p, st);

@@ -342,3 +342,58 @@ def test_graph_and_other_stream():
         side.synchronize()
         for a, b in zip(other, eager):
             assert torch.equal(a, b)
+
+
+def _scales_of(amax):
+    """The 32-bit quotient by 448 (by a tensor: a number's reciprocal would be multiplied by)."""
+    return amax.clamp_min(2.0 ** -110) / torch.full_like(amax, 448.0)
+
+
+# A launch counts its threads in 32 bits: 2^24 - 1 workgroups of 256, 2^23 - 1 of 512.  What is more goes into further launches.
+def test_more_rows_than_a_launch_takes():
+    """16 threads to a row: 2^28 - 16 rows."""
+    rows = (1 << 28) - 16 + 37
+    x = torch.randint(-1, 2, (rows, 1), device="cuda", dtype=torch.int8).bfloat16()
+    q, s = ops.quantize(x)
+    top = torch.where(x == 0, torch.zeros((), device="cuda"), torch.full((), 448.0, device="cuda")) * x
+    for a in range(0, rows, 1 << 26):
+        assert torch.equal(q[a:a + (1 << 26), :1].float(), top[a:a + (1 << 26)])
+    assert int(q[-5000:, 1:].view(torch.uint8).amax()) == 0
+    assert torch.equal(s[0], _scales_of(x[:, 0].float().abs()))
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_more_tiles_than_a_launch_takes(block_rows):
+    """A workgroup to 128 rows: (2^24 - 1) * 128 of them."""
+    whole = ((1 << 24) - 1) * 128
+    rows = whole + 5
+    x = torch.zeros((rows, 1), dtype=torch.bfloat16, device="cuda")
+    x[:: 77] = 3.0
+    x[-300:] = _normal(1, 300, 1, dtype=torch.bfloat16)
+    q, s = ops.quantize(x, block_rows, rows=False, transposed=True)
+    amax = torch.cat([x[:whole].view(-1, 128).abs().amax(1), x[whole:].abs().amax()[None]]).float()
+    assert torch.equal(s[:, 0], _scales_of(amax))
+    tail = ops.quantize(x[whole - 640:].clone(), block_rows, rows=False, transposed=True)
+    assert torch.equal(q[:, whole - 640:].view(torch.uint8), tail[0].view(torch.uint8)) and torch.equal(s[-6:], tail[1])
+
+
+def test_more_rows_of_b_than_a_launch_takes():
+    """16 rows of B to a workgroup of 512: 2^27 - 128 rows."""
+    edge = (1 << 27) - 128
+    n, k = edge + 200, 128
+    codes = torch.zeros((n, k), dtype=torch.uint8, device="cuda")
+    codes[edge - 256:] = torch.randint(0, 0x70, (456, k), device="cuda", dtype=torch.uint8)
+    scales = torch.rand((1, -(-n // 128)), device="cuda") + 0.5
+    x = _normal(1, 2, k, dtype=torch.bfloat16)
+    y = ops.linear(x, codes.view(ops.E4M3), scales)
+    assert float(y[:, :edge - 256].abs().amax()) == 0.0
+    assert torch.equal(y[:, edge - 256:], ops.linear(x, codes[edge - 256:].view(ops.E4M3), scales[:, edge // 128 - 2:].contiguous()))
+
+
+def test_more_zeros_than_a_launch_takes():
+    """A product over nothing with 5 * 2^30 groups of four zeros."""
+    m, n = (1 << 30) + 3, 17
+    out = torch.ones((m, n), dtype=torch.bfloat16, device="cuda")
+    a, b = (torch.empty((r, 0), dtype=ops.E4M3, device="cuda") for r in (m, n))
+    ops.matmul(a, torch.empty((0, m), device="cuda"), b, torch.empty((0, n), device="cuda"), 0, out=out)
+    assert float(out.amax()) == 0.0
