@@ -388,6 +388,14 @@ __global__ __launch_bounds__(kGradThreads) void k_norm_grad(Bwd p) {
     }
     if (pre) { nqm = p.pre_stats[row]; nqr = p.pre_stats[p.rows + row]; }
   };
+  // A group past the row holds the row's first elements, and its weights are zero:
+  // it adds nothing to a sum, unless what it holds is not finite.
+  auto only_in_row = [&](int j, float a[2], const float before[2]) {
+    if (kVec && have[j] <= 0) {
+      a[0] = before[0];
+      a[1] = before[1];
+    }
+  };
   // (the last row of the gate may have fewer tokens than chunks for them)
   constexpr bool kAhead = !(kLayer && kN > kHold);   // registers for a row more
   if (kAhead && r0 < r1) fetch(r0);
@@ -424,12 +432,14 @@ __global__ __launch_bounds__(kGradThreads) void k_norm_grad(Bwd p) {
           dqw[j][i] += u[j][i] * hat[j][i];
         }
         side_add(0, j, u[j]);
+        const float before[2] = {a[0], a[1]};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           u[j][i] *= kN > kHold ? w[i] : kept_qw[kN > kHold ? 0 : j][i];
           a[0] += u[j][i] * hat[j][i];
           if constexpr (kLayer) a[1] += u[j][i];
         }
+        only_in_row(j, a, before);
       }
       row_sum<kLayer ? 2 : 1>(a, red, waves, wave, 0, half);
       const float a0 = a[0] * inv * qr, a1 = kLayer && p.pre == SIM_NORM_LAYER ? a[1] * inv : 0.0f;
@@ -469,12 +479,14 @@ __global__ __launch_bounds__(kGradThreads) void k_norm_grad(Bwd p) {
         q[j][i] += d[j][i] * y[j][i];
       }
       side_add(1, j, d[j]);
+      const float before[2] = {a[0], a[1]};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         d[j][i] *= kN > kHold ? w[i] : kept_gw[kN > kHold ? 0 : j][i];
-        a[0] += d[j][i] * y[j][i];                   // (the weights are zero past the row)
+        a[0] += d[j][i] * y[j][i];
         if constexpr (kLayer) a[1] += d[j][i];
       }
+      only_in_row(j, a, before);
     }
     if (post) {
       row_sum<kLayer ? 2 : 1>(a, red, waves, wave, 0, half);

@@ -340,3 +340,36 @@ def test_padding_of_not_finite_rows(hidden, kind):
     # zero rows with eps = 0 are 0 / 0
     q = ops.norm_block(y, pre=kind, eps=0.0, quantized=True, pre_bias=_normal(2, hidden))
     assert torch.isnan(q.x[:, :hidden].float()).all() and int(q.x[:, hidden:].view(torch.uint8).amax()) == 0
+
+
+@pytest.mark.parametrize("hidden", [131, 200, 1000, 4104, 8200, 12296])
+@pytest.mark.parametrize("post,pre", [("rms", "none"), ("layer", "none"), ("rms", "rms"), ("none", "layer")])
+def test_infinite_gradients(hidden, post, pre):
+    """An infinity anywhere in a row of a gradient gives what the formula gives for it, its lanes past the row's end included."""
+    c = _case(4, hidden, post, pre, "none", torch.float32, torch.float32, seed=31)
+    stats = dict(post_stats=_stats(c["y"].double(), post), pre_stats=_stats(c["h"].double(), pre))
+    dh, dx = _normal(5, 4, hidden), _normal(6, 4, hidden) if pre != "none" else None
+    kw = dict(post_weight=c["pw"], pre_weight=c["qw"], post=post, pre=pre, **stats)
+    clean = ops.norm_block_backward(dh, dx, c["h"], c["y"], **kw)
+    for at in (0, 3, hidden - 1):
+        up = dx if dx is not None else dh
+        bad = up.clone()
+        bad[1, at] = float("inf")
+        g = ops.norm_block_backward(dh if dx is not None else bad, bad if dx is not None else None, c["h"], c["y"], **kw)
+        for key in ("dh", "dy"):
+            got, was = getattr(g, key), getattr(clean, key)
+            assert torch.equal(got[[0, 2, 3]], was[[0, 2, 3]])
+        # the mean of u hat is infinite, as that of u is: minus hat times it, or NaN where both infinities meet
+        side = "post" if dx is None else "pre"
+        mean, rstd = (stats[side + "_stats"].double()[i, :, None] for i in range(2))
+        v = c["y"] if dx is None else c["h"]
+        hat = (v.double() - mean) * rstd
+        u = bad.double() * c["pw" if dx is None else "qw"].double()
+        want = u - hat * (u * hat).mean(1, keepdim=True)
+        if (post if dx is None else pre) == "layer":
+            want = want - u.mean(1, keepdim=True)
+        want = (want * rstd)[1]
+        got = (g.dy if dx is None else g.dh - dh)[1].double()
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        infinite = torch.isinf(want)
+        assert infinite.any() and torch.equal(got[infinite], want[infinite])
