@@ -326,7 +326,7 @@ py::tuple norm_backward(const Maybe& dh, const Maybe& dx, const Tensor& h, const
   a.dh = out.data_ptr(); a.ld_dh = m.cols;
   // a bias has a gradient after a layer norm, and wherever the forward pass took one (its values count in dgate alone)
   const bool post_sum = post == SIM_NORM_LAYER || (post != SIM_NORM_NONE && a.post_bias);
-  const bool pre_sum = pre == SIM_NORM_LAYER || (pre != SIM_NORM_NONE && vector_of(at, pre_bias, m.cols, "pre_bias"));
+  const bool pre_sum = (vector_of(at, pre_bias, m.cols, "pre_bias") && pre != SIM_NORM_NONE) || pre == SIM_NORM_LAYER;
   const bool wanted[4] = {post != SIM_NORM_NONE, post_sum, pre != SIM_NORM_NONE, pre_sum};
   float** places[4] = {&a.dpost_weight, &a.dpost_bias, &a.dpre_weight, &a.dpre_bias};
   for (int i = 0; i < 4; ++i)

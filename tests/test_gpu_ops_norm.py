@@ -373,3 +373,15 @@ def test_infinite_gradients(hidden, post, pre):
         assert torch.equal(torch.isnan(got), torch.isnan(want))
         infinite = torch.isinf(want)
         assert infinite.any() and torch.equal(got[infinite], want[infinite])
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_parameters_of_another_size_are_refused(kind):
+    h, w, wrong = _normal(1, 4, 64), _normal(2, 64), _normal(3, 63)
+    f = ops.norm_block(h, h, post=kind, pre=kind)
+    for name in ("post_weight", "post_bias", "pre_weight", "pre_bias"):
+        for bad in (wrong, w.double(), w.cpu()):
+            with pytest.raises(ValueError):
+                ops.norm_block(h, h, post=kind, pre=kind, **{name: bad})
+            with pytest.raises(ValueError):
+                ops.norm_block_backward(h, h, f.h, h, post_stats=f.post_stats, pre_stats=f.pre_stats, post=kind, pre=kind, **{name: bad})
