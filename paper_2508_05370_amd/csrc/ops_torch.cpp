@@ -4,6 +4,7 @@
 // (ops.py is its face), so that the library itself knows no torch; as native
 // code because a call on one token takes the card 3 us.
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/utils/pybind.h>
@@ -72,17 +73,26 @@ int type_of(const Tensor& t, const char* what) {
 void* ptr(const Tensor& t) { return t.data_ptr(); }
 void* ptr(const Maybe& t) { return t ? t->data_ptr() : nullptr; }
 
+// Results have no history: a tensor whose gradient autograd is to record is
+// refused, as an out argument of torch's own functions does.
+void require_unrecorded(const Tensor& t) {
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    refuse("a tensor requires its gradient, which these calls do not record: pass it detached, or call under torch.no_grad()");
+}
+
 // Tensors are on the current GPU; its current stream.
 struct Place {
   c10::Device device;
   void* stream;
-  explicit Place(const Tensor& t) : device(t.device()), stream(nullptr) {
+  explicit Place(const Tensor& t, bool parameters = false) : device(t.device()), stream(nullptr) {
+    if (!parameters) require_unrecorded(t);
     if (!t.is_cuda()) refuse("tensors must be on a GPU, not on " + device.str());
     const auto s = c10::hip::getCurrentHIPStream();
     if (s.device_index() != device.index()) refuse("tensors must be on the current GPU, not on " + device.str());
     stream = s.stream();
   }
   void on(const Tensor& t) const {
+    require_unrecorded(t);
     if (t.device() != device) refuse("tensors on " + device.str() + " and " + t.device().str());
   }
   void on(const Maybe& t) const {
@@ -360,7 +370,7 @@ void adamw(const List& p, const List& g, const List& m, const List& v, const std
   for (const List* l : lists) require(!l || l->size() == n, "lists of one length");
   require(decays.size() == 1 || decays.size() == n, "one weight decay, or one for each tensor");
   if (n == 0) return;
-  const Place at(p[0]);
+  const Place at(p[0], true);   // (parameters require gradients: a step on them is no part of what is recorded)
   for (const List* l : lists) {
     if (!l) continue;
     const at::ScalarType type = (*l)[0].scalar_type();

@@ -6,6 +6,10 @@ there is no host fallback.  Checks and calls are native (csrc/ops_torch.cpp,
 built in-tree as _ops.so): a call on one token takes the card 3 us.  A wrong
 type, shape or device raises ValueError; what the library refuses raises
 binding.SimError.
+
+Autograd does not see these calls: gradients are the *_backward calls' results.
+So a tensor that requires its gradient is refused (ValueError) while autograd
+records, adamw's lists excepted: pass it detached, or call under torch.no_grad().
 """
 import collections
 import os

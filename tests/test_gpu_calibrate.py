@@ -65,3 +65,28 @@ def test_command(capsys):
     calibrate.main(["--model", "llama-7b", "--tp", "8", "--tokens", "512", "--plans", "8192", "--nodes", "8"])
     out = json.loads(capsys.readouterr().out)
     assert out["best_plan"] >= 0 and out["rates"]["tflops"] > 1
+
+
+def test_no_history_is_lost_silently():
+    """What autograd records is refused by every argument; the same calls under no_grad, and on detached tensors, are as ever."""
+    from paper_2508_05370_amd import ops
+    g = torch.Generator(device="cuda").manual_seed(5)
+    h, y, x, w = (torch.randn(*s, generator=g, device="cuda") for s in ((6, 256), (6, 256), (6, 256), (256,)))
+    codes, scales = ops.quantize(x, 128)
+    norms = dict(h=h, y=y, gate=torch.ones_like(w), post_weight=w, post_bias=w, pre_weight=w, pre_bias=w)
+    f = ops.norm_block(post="rms", pre="layer", **norms)
+    back = dict(norms, dh=y, dx=x, h=f.h, post_stats=f.post_stats, pre_stats=f.pre_stats)
+    for call, kw in ((lambda **k: ops.norm_block(post="rms", pre="layer", **k), dict(norms, out=torch.empty_like(h))),
+                     (lambda **k: ops.norm_block_backward(post="rms", pre="layer", **k), back),
+                     (ops.linear, dict(x=x, codes=codes, scales=scales, out=torch.empty(6, 6, device="cuda"))),
+                     (lambda **k: ops.matmul(k=256, **k), dict(a=codes, a_scales=scales, b=codes, b_scales=scales,
+                                                               out=torch.empty(6, 6, device="cuda")))):
+        call(**kw)
+        for name in kw:
+            if kw[name].dtype == ops.E4M3:
+                continue
+            recorded = dict(kw, **{name: kw[name].detach().clone().requires_grad_()})
+            with pytest.raises(ValueError, match="no_grad"):
+                call(**recorded)
+            with torch.no_grad():
+                call(**recorded)

@@ -219,3 +219,23 @@ def test_tensors_are_refused():
     with pytest.raises(ValueError, match="e4m3"):
         torch_ops.linear(x, x, x)
     torch_ops.adamw([], [], [], [], step=1, lr=1e-3)
+
+
+def test_recorded_tensors_are_refused():
+    """No call leaves a history, so none takes a tensor whose gradient is being recorded (on which device it is does not matter)."""
+    x, w = torch.zeros(4, 128), torch.zeros(128)
+    leaf, inner = torch.zeros(4, 128, requires_grad=True), torch.zeros(4, 128, requires_grad=True) * 2.0
+    codes, scales = torch.zeros(8, 128, dtype=torch_ops.E4M3), torch.zeros(1, 8)
+    for bad in (leaf, inner):
+        for call in (lambda: torch_ops.quantize(bad), lambda: torch_ops.linear(bad, codes, scales), lambda: torch_ops.norm_block(bad),
+                     lambda: torch_ops.norm_block(bad, x), lambda: torch_ops.linear_forward(bad, x),
+                     lambda: torch_ops.norm_block_backward(None, x, bad, pre_stats=torch.zeros(2, 4))):
+            with pytest.raises(ValueError, match="no_grad"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+                call()
+    with pytest.raises(ValueError, match="GPU"):
+        torch_ops.quantize(inner.detach())
+    # an optimizer step writes to parameters
+    with pytest.raises(ValueError, match="GPU"):
+        torch_ops.adamw([leaf], [x], [x], [x], step=1, lr=1e-3)
