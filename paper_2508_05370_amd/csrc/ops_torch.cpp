@@ -80,6 +80,12 @@ void require_unrecorded(const Tensor& t) {
     refuse("a tensor requires its gradient, which these calls do not record: pass it detached, or call under torch.no_grad()");
 }
 
+// The library writes through pointers: autograd is told, so that it notices a
+// tensor that it saved.  (Tensors of inference mode have no counter.)
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Tensors are on the current GPU; its current stream.
 struct Place {
   c10::Device device;
@@ -178,6 +184,7 @@ Tensor matmul(const Tensor& a, const Tensor& a_scales, const Tensor& b, const Te
   const size_t size = L.matmul_workspace(m, n, k);
   const Tensor ws = at.bytes(size);
   check(L.matmul(&ba, &bb, m, n, k, o.p, o.type, o.ld, accumulate, ptr_or_null(ws), size, at.stream), "sim_op_matmul");
+  if (out) written(c);
   return c;
 }
 
@@ -195,6 +202,7 @@ Tensor linear(const Tensor& x, const Tensor& codes, const Tensor& scales, const 
   const size_t size = L.linear_workspace(m.rows, n, m.cols);
   const Tensor ws = at.bytes(size);
   check(L.linear(m.p, m.type, m.ld, &w, m.rows, n, m.cols, o.p, o.ld, ptr_or_null(ws), size, at.stream), "sim_op_linear");
+  if (out) written(y);
   return y;
 }
 
@@ -281,6 +289,7 @@ py::tuple norm(const Tensor& h, const Maybe& y, const Maybe& gate, const Maybe& 
     require(!quantized, "quantized needs pre");
   }
   if (m.rows) check(L.norm(&a, at.stream), "sim_op_norm");
+  if (out) written(sum);
   auto give = [](const Tensor& t) { return t.defined() ? py::cast(t) : py::object(py::none()); };
   return py::make_tuple(sum, give(x), give(x_scale), give(post_stats), give(pre_stats));
 }
@@ -404,6 +413,10 @@ void adamw(const List& p, const List& g, const List& m, const List& v, const std
                 (float)decays[decays.size() == 1 ? 0 : i]};
     first += (uint64_t)(blocks * SIM_BLOCK);
   }
+  // (a failed call may have begun: all lists but the gradients' count as written)
+  for (const List* l : lists)
+    if (l && l != &g)
+      for (const Tensor& t : *l) written(t);
   check(L.adamw(table.data(), (int64_t)n, &a, at.stream), "sim_op_adamw");
 }
 

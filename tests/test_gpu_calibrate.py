@@ -90,3 +90,41 @@ def test_no_history_is_lost_silently():
                 call(**recorded)
             with torch.no_grad():
                 call(**recorded)
+
+
+def test_writes_are_seen_by_autograd():
+    """What a call writes into counts as changed: a saved tensor that was overwritten is an error in backward, as after torch's own
+    in-place functions."""
+    from paper_2508_05370_amd import ops
+    x = torch.ones(4, 256, device="cuda")
+    q, s = ops.quantize(x)
+
+    def writes(t, call):
+        before = t._version
+        call()
+        assert t._version > before
+    out = torch.zeros(4, 4, device="cuda")
+    writes(out, lambda: ops.matmul(q, s, q, s, 256, out=out))
+    writes(out, lambda: ops.linear(x, q, s, out=out))
+    out = torch.zeros(4, 256, device="cuda")
+    writes(out, lambda: ops.norm_block(x, x, out=out))
+    reads = [t._version for t in (x, q, s)]
+    for bits in (32, 8):
+        p, g, copy = (torch.ones(256, device="cuda") for _ in range(3))
+        m, v, scales = [torch.zeros(256, device="cuda") for _ in range(2)], None, {}
+        if bits == 8:
+            m, v = zip(*(ops.quantize(t[None]) for t in m))
+            m, v = [t[0] for t in m], [t[:, 0] for t in v]
+            scales = dict(exp_avg_scales=v[:1], exp_avg_sq_scales=v[1:])
+        for t in (p, copy, *m, *(v or ())):
+            writes(t, lambda: ops.adamw([p], [g], m[:1], m[1:], copies=[copy], step=1, lr=1e-3, **scales))
+        assert g._version == 0
+    assert reads == [t._version for t in (x, q, s)]
+    w = torch.nn.Parameter(torch.ones(256, device="cuda"))
+    loss = w.square().sum()
+    ops.adamw([w], [g], [torch.zeros_like(g)], [torch.zeros_like(g)], step=1, lr=1e-3)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():          # (tensors without a counter)
+        out = torch.zeros(4, 4, device="cuda")
+        ops.matmul(q, s, q, s, 256, out=out)
