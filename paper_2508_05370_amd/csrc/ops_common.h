@@ -35,9 +35,11 @@ inline int type_bytes(int dtype) { return dtype == SIM_FP32 ? 4 : dtype == SIM_B
 // read and the rest are zero.
 template <typename T>
 struct Raw {
-  typedef T t8 __attribute__((ext_vector_type(8)));
+  // (16 bytes are what callers make sure of, for 32-bit elements too)
+  typedef T t8 __attribute__((ext_vector_type(8), aligned(16)));
   t8 v;
 };
+static_assert(alignof(Raw<float>::t8) == 16 && alignof(Raw<bf16>::t8) == 16, "an access of eight elements asks for 16 bytes' alignment");
 // (a 32-bit column's place is a 32-bit number of bytes, so that the row's
 // address stays in scalar registers)
 template <typename T, typename I>
