@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2508_05370_amd import ops
+import ops_abi
 
 pytestmark = pytest.mark.gpu
 # unit of the last place of the output types
@@ -385,3 +386,63 @@ def test_parameters_of_another_size_are_refused(kind):
                 ops.norm_block(h, h, post=kind, pre=kind, **{name: bad})
             with pytest.raises(ValueError):
                 ops.norm_block_backward(h, h, f.h, h, post_stats=f.post_stats, pre_stats=f.pre_stats, post=kind, pre=kind, **{name: bad})
+
+
+VIEWS = [(256, 0, 8), (256, 1, 0), (256, 4, 4), (250, 0, 0), (251, 3, 2), (4104, 8, 16), (12296, 1, 8)]
+
+
+def _view(seed, rows, hidden, offset, pad, dtype, scale=1.0):
+    """A buffer with a matrix in it that starts and goes on anywhere."""
+    buf = _normal(seed, offset + rows * (hidden + pad) + 8, dtype=dtype, scale=scale)
+    return buf, buf[offset:].as_strided((rows, hidden), (hidden + pad, 1))
+
+
+@pytest.mark.parametrize("hidden,offset,pad", VIEWS)
+@pytest.mark.parametrize("act,res", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_backward_views_and_in_place(hidden, offset, pad, act, res, kind):
+    """Strided and misaligned rows give what contiguous ones do; dh may take dh_out's place; nothing beside the outputs is written."""
+    rows = 9
+    _, h = _view(1, rows, hidden, offset, pad, res)
+    _, y = _view(2, rows, hidden, offset + 1, pad, act)
+    _, dx = _view(3, rows, hidden, offset, pad + 1, act)
+    dh_buf, dh = _view(4, rows, hidden, offset, pad, res)
+    dy_buf, dy = _view(5, rows, hidden, offset, pad + 8, act)
+    w, stats = 1.0 + _normal(6, hidden, scale=0.2), dict(post_stats=_stats(y.double(), kind), pre_stats=_stats(h.double(), kind))
+    kw = dict(post_weight=w, pre_weight=w, post=kind, pre=kind, alpha=0.9, beta=0.7, **stats)
+    # the formula in 64 bits: through the pre norm of the held sum, then through the sum
+    leaf, qw, qb = h.double().requires_grad_(), w.double().requires_grad_(), torch.zeros(hidden, device="cuda").double().requires_grad_()
+    ((_norm64(leaf, kind) * qw + qb) * dx.double()).sum().backward()
+    c = dict(h=h, y=y, gate=None, pw=w, pb=torch.zeros(hidden, device="cuda"), qw=None, qb=None, per=rows)
+    want = _grad64(c, kind, "none", 0.9, 0.7, dh.double() + leaf.grad, None)[1]
+    terms = 8.0 + float(want["h"].abs().amax()) + float(want["y"].abs().amax())
+    sums = 4.0 * terms * terms * (rows ** 0.5 + 4.0)           # as in test_backward
+    got = ops.norm_block_backward(dh, dx, h, y, **kw)
+    _close(got.dh, want["h"], ULP[res], terms)
+    _close(got.dy, want["y"], ULP[act], terms)
+    _close(got.dpost_weight, want["pw"], ULP[torch.float32], sums)
+    _close(got.dpre_weight, qw.grad, ULP[torch.float32], sums)
+    if kind == "layer":
+        _close(got.dpost_bias, want["pb"], ULP[torch.float32], sums)
+        _close(got.dpre_bias, qb.grad, ULP[torch.float32], sums)
+    # the library itself, dh in dh_out's place
+    types = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    k = {"rms": 1, "layer": 2}[kind]
+    kept = dh_buf.clone(), dy_buf.clone()
+    size = ops_abi.lib().sim_op_norm_backward_workspace(rows, hidden, rows)
+    ws, sums_out = torch.empty(size, dtype=torch.uint8, device="cuda"), [torch.empty(hidden, device="cuda") for _ in range(2)]
+    a = ops_abi.NormGradArgs(rows=rows, hidden=hidden, act=types[act], res=types[res], post=k, pre=k, alpha=0.9, beta=0.7,
+                             dh_out=dh.data_ptr(), ld_dh_out=dh.stride(0), dx=dx.data_ptr(), ld_dx=dx.stride(0), h=h.data_ptr(),
+                             ld_h=h.stride(0), y=y.data_ptr(), ld_y=y.stride(0), rows_per_gate=rows, post_weight=w.data_ptr(),
+                             pre_weight=w.data_ptr(), post_stats=stats["post_stats"].data_ptr(), pre_stats=stats["pre_stats"].data_ptr(),
+                             dh=dh.data_ptr(), ld_dh=dh.stride(0), dy=dy.data_ptr(), ld_dy=dy.stride(0),
+                             dpost_weight=sums_out[0].data_ptr(), dpre_weight=sums_out[1].data_ptr())
+    assert ops_abi.lib().sim_op_norm_backward(ops_abi.C.byref(a), ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    _close(dh, want["h"], ULP[res], terms)
+    _close(dy, want["y"], ULP[act], terms)
+    for got, true in zip(sums_out, (want["pw"], qw.grad)):
+        _close(got, true, ULP[torch.float32], sums)
+    for buf, was, out in ((dh_buf, kept[0], dh), (dy_buf, kept[1], dy)):
+        was[out.storage_offset():].as_strided(out.shape, out.stride()).copy_(out)
+        assert torch.equal(buf, was)

@@ -397,3 +397,40 @@ def test_more_zeros_than_a_launch_takes():
     a, b = (torch.empty((r, 0), dtype=ops.E4M3, device="cuda") for r in (m, n))
     ops.matmul(a, torch.empty((0, m), device="cuda"), b, torch.empty((0, n), device="cuda"), 0, out=out)
     assert float(out.amax()) == 0.0
+
+
+def test_tiled_product_past_32_bits():
+    """Codes, outputs and transposes further than 2^31 elements into their tensors, with more rows than the streaming form takes."""
+    m, k = 70000, 32768
+    big = torch.zeros((m, k), dtype=torch.bfloat16, device="cuda")
+    big[-200:] = _normal(3, 200, k, dtype=torch.bfloat16)
+    q, s, qt, st = ops.quantize(big, transposed=True)
+    tail = big[-(m % 128 + 128):].clone()               # the last whole block of rows, and the rest
+    q1, s1, qt1, st1 = ops.quantize(tail, transposed=True)
+    r = tail.shape[0]
+    assert torch.equal(q[-r:].view(torch.uint8), q1.view(torch.uint8)) and torch.equal(s[:, -r:], s1)
+    assert torch.equal(qt[:, -256:].view(torch.uint8), qt1.view(torch.uint8)) and torch.equal(st[-2:], st1)
+    b, sb = _blocks(5, 96, k, 128)
+    y = ops.matmul(q, s, b, sb, k, torch.float32)
+    want = ops.dequantize(q[-200:], s[:, -200:], k).double() @ ops.dequantize(b, sb, k).double().t()
+    # as in test_matmul_many_tiles
+    assert float((y[-200:].double() - want).norm() / want.norm()) < 6e-5 and float(y[:-r].abs().amax()) == 0.0
+    del big, qt, st, y
+    c, sc = _blocks(6, 33000, 128, 128)
+    d, sd = _blocks(7, m, 128, 1)
+    y = ops.matmul(d, sd, c, sc, 128, torch.bfloat16)
+    want = ops.dequantize(d[-3:], sd[:, -3:], 128).double() @ ops.dequantize(c, sc, 128).double().t()
+    assert float((y[-3:].double() - want).norm() / want.norm()) < 4e-3
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 40, 200])
+@pytest.mark.parametrize("hidden", [256, 1000, 4096, 8200])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_norm_into_product(tokens, hidden, kind):
+    """A norm's output in 8 bits is the operand of a product as it is: the next linear layer without a pass of its own over x."""
+    h, y = _normal(1, tokens, hidden, dtype=torch.bfloat16), _normal(2, tokens, hidden, dtype=torch.bfloat16)
+    f = ops.norm_block(h, y, pre_weight=1.0 + _normal(3, hidden, scale=0.2), post=kind, pre=kind, quantized=True)
+    w, ws = _blocks(4, 130, hidden, 128, 0.02)
+    want, loss = _product64(f.x, f.x_scale, w, ws, hidden)
+    got = ops.matmul(f.x, f.x_scale, w, ws, hidden, torch.bfloat16)
+    assert ((got.double().cpu() - want).abs() <= loss + want.abs() * ULP[torch.bfloat16]).all()
