@@ -9,6 +9,11 @@ tensor-parallel group holds, takes the two rates from the time of its products
 and of its norms, and evaluates random plans of the model on a cluster of such
 devices beside ones half as fast.
 
+What the figures are: the TFLOP/s are those of 8-bit products with the rounding
+of their operands, while the evaluator counts the model's bytes per element as
+its description gives them; and the optimizer step's time is printed, but no
+plan's time contains one.
+
     python -m paper_2508_05370_amd.calibrate --model llama-70b --tp 8
 
 It prints one JSON line.

@@ -7,6 +7,18 @@
 // 16-bit data.  Thread t of a row's T threads holds the groups of eight
 // neighbours t, t + T, ...: 16-byte accesses, and 16 neighbouring threads hold
 // one block of 128 for the output in 8 bits.
+//
+// Two kinds of rows take several times what their bytes do.  Ones that are not
+// whole multiples of eight elements, or do not start at 16 bytes, go one element
+// at a time (kVec false): 8192 x 8191 forward 332 us and backward 458, where 8192 x
+// 8192 take 115 and 169; 4096 x 4099 95 and 134, for 24.5 and 42.  And long ones,
+// with more groups per thread than the registers hold, spill: backward from 8193
+// channels on (layer norms a little from 4097 on), forward from 16385 on (with a
+// stream in 32 bits a little from 12289 on).  By the
+// compiler's report a lane of the backward pass keeps 15 to 112 registers in
+// memory at up to 12288 channels (4096 rows, RMS: 167 us, 3.6 TB/s), 109 to 280 at
+// up to 16384 (444 us, 1.8 TB/s) and 611 to 1329 beyond (2048 x 32768 1188 us, 0.7
+// TB/s; forward, with up to 449, 336 us).
 #include <type_traits>
 
 #include "ops_common.h"
@@ -100,8 +112,9 @@ __device__ inline void moments(float v[kN][8], const int have[kN], int kind, flo
 
 // A workgroup takes rows_each rows one after another for each group of
 // `per_row` threads, the next row on its way while one is worked on.  8192 x 8192
-// in 16 bits, x in 8: 114 us, 4.1 TB/s of 7 B per element (one row to a
-// workgroup and branches around what is past the row: 136 to 159).
+// in 16 bits: 115 us, 4.7 TB/s of 8 B per element, and with x in 8 bits 110, 4.3
+// TB/s of 7 B (one row to a workgroup and branches around what is past the row:
+// 136 to 159).
 template <typename A, typename R, int kN, bool kVec>
 __global__ __launch_bounds__(kThreads) void k_norm(Fwd p, int per_row, int rows_each) {
   __shared__ float red[32];
@@ -279,8 +292,8 @@ enum { kDqw, kDqb, kQ, kP, kSums };
 // has a bias; the two sums more that this takes are kept in LDS where registers
 // would not hold them (every thread has its own places there).  kFull: both
 // norms, and all inputs and outputs but the sums, are there.
-// 8192 x 8192 in 16 bits: 162 us, 5.0 TB/s of 12 B per element; 2047 x 12288
-// layer norms with the stream in 32 bits 130 us, 3.5 TB/s, where the registers
+// 8192 x 8192 in 16 bits: 165 us, 4.9 TB/s of 12 B per element; 2047 x 12288
+// layer norms with the stream in 32 bits 135 us, 3.4 TB/s, where the registers
 // do not hold a row ahead as well (with one, spilled: 178).
 constexpr int kGradThreads = 512;
 
@@ -576,7 +589,7 @@ __global__ __launch_bounds__(kGradThreads) void k_norm_grad(Bwd p) {
 
 // Sums over chunks: a workgroup takes 64 columns of one run of chunks (those of
 // one row of the gate, or all), wave w of its 16 every 16th chunk (256 chunks of
-// 8192 columns: 6.5 us); with more workgroups than the card holds of 16 waves
+// 8192 columns: 6.7 to 7.6 us); with more workgroups than the card holds of 16 waves
 // it has 8 (12288 columns, 4 runs of 64 chunks: 11.6 us, with 16 waves 15.6).
 // The first pass, for each row of the gate, finishes that row's gradient and
 // leaves the run's sums, times the gate, in the run's first chunk; the second
