@@ -88,6 +88,8 @@ typedef struct {
  * codes == NULL: not wanted.  Both have the same block_rows: with 1 the
  * transpose's blocks are 128 rows of one column of X; with 128 both share
  * the codes and the scales are transposed.  rows = 0 or cols = 0: no-op.
+ * rows and cols are below 2^31; 2^31 - 128 columns are the most, unless rows
+ * alone are wanted with block_rows 1.
  */
 int sim_op_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, const sim_blocks* q,
                     const sim_blocks* qt, void* stream);

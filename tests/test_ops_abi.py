@@ -239,3 +239,12 @@ def test_recorded_tensors_are_refused():
     # an optimizer step writes to parameters
     with pytest.raises(ValueError, match="GPU"):
         torch_ops.adamw([leaf], [x], [x], [x], step=1, lr=1e-3)
+
+
+def test_more_columns_than_a_launch_takes():
+    """Tiles of one row's worth of columns are not split over launches: refused before any."""
+    cols = (1 << 31) - 127
+    for block_rows in (1, 128):
+        q, qt = _blocks(1, cols, block_rows=block_rows), _blocks(cols, 1, block_rows=block_rows)
+        assert _quantize(rows=1, cols=cols, ld=cols, q=q, qt=qt) == B.SIM_EINVAL
+    assert _quantize(rows=1, cols=1 << 31, ld=1 << 31, q=_blocks(1, 1 << 31)) == B.SIM_EINVAL
